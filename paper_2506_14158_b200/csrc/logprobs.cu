@@ -43,6 +43,7 @@ struct LpParams {
     const int32_t* next_token;
     int entries, T, V, top;
     float scale, inv_scale;    // log2(e) / temperature, and its reciprocal
+    double exact;              // log2(e) / temperature, where it or its reciprocal is too small for float32 too
     float* logprob;
     float* entropy;
     int32_t* top_token;
@@ -215,17 +216,17 @@ __device__ __forceinline__ void lp_move(float M, float& S, float& E, float to) {
     E = f == 0.0f ? 0.0f : (E + S * d) * f, S = f == 0.0f ? 0.0f : S * f;
 }
 
-// Rows whose greatest logit times log2(e) / tau has a rounding of more than a few powers of two, or leaves float32: S and E by differences
-// against the exact maximum, all of the row by one block.
+// Rows whose greatest logit times log2(e) / tau has a rounding of more than a few powers of two, or leaves float32, and temperatures at which
+// the clamp of LpSums does (beyond 1e-30 .. 1e30): S and E by differences against the exact maximum, in float64, all of the row by one block.
 template <typename T, int S>
-__device__ __noinline__ void lp_extreme(const Row<T> row, LpShared<S>& sh, float m, float c, float& sum, float& weighted) {
+__device__ __noinline__ void lp_extreme(const Row<T> row, LpShared<S>& sh, float m, double c, float& sum, float& weighted) {
     float s = 0.0f, e = 0.0f;
     for (int i = threadIdx.x; i < row.n; i += blockDim.x) {
         float x[Vec<T>::E];
         Vec<T>::unpack(row.load(i), x);
 #pragma unroll
         for (int j = 0; j < Vec<T>::E; ++j) {
-            const float y = fmaxf((x[j] - m) * c, -200.0f), t = exp2_fast(y);
+            const float y = (float)fmax(((double)x[j] - m) * c, -200.0), t = exp2_fast(y);
             s += t, e += t * y;
         }
     }
@@ -440,9 +441,9 @@ logprobs_kernel(const LpParams p, int cluster, int per) {
     m = M = -INFINITY, s = e = 0.0f;
     for (int b = 0; b < cluster; ++b) m = max_nan(m, sh.part[b].x), M = fmaxf(M, sh.part[b].y);
     if (!usable(m)) return undefined(NAN, S4C_SEQ_NONFINITE);
-    const bool extreme = !(fabsf(m) < 1e37f) || !(fabsf(m * c) < 1e8f);
+    const bool extreme = !(fabsf(m) < 1e37f) || !(fabsf(m * c) < 1e8f) || !(c > 1e-30f && c < 1e30f);
     if (extreme) {
-        lp_extreme(row, sh, m, c, s, e);
+        lp_extreme(row, sh, m, p.exact, s, e);
     } else {
         for (int b = 0; b < cluster; ++b) {
             float4 q = sh.part[b];
@@ -453,7 +454,7 @@ logprobs_kernel(const LpParams p, int cluster, int per) {
     if (tid >= max(1, cluster * top)) return;
     const float ln_s = ln_series(s);
     // (in float64: x c may leave float32 where the log probability does not)
-    auto logprob = [&](float x) { return (float)((extreme ? ((double)x - m) * c : (double)x * c - M) * kLn2 - ln_s); };
+    auto logprob = [&](float x) { return (float)((extreme ? ((double)x - m) * p.exact : (double)x * c - M) * kLn2 - ln_s); };
     const bool in_range = w.token >= 0 && w.token < p.V;
     if (tid == 0) {
         if (p.logprob) p.logprob[r] = in_range ? logprob(Vec<T>::get(row.x + w.token)) : NAN;
@@ -522,7 +523,7 @@ extern "C" s4c_status s4c_token_logprobs(const void* logits, long long row_strid
     if (dt != S4C_F32 && dt != S4C_BF16) return S4C_ERR_DTYPE;
     if (top > kLpMaxTop) return S4C_ERR_UNSUPPORTED;
     if (reinterpret_cast<uintptr_t>(logits) % dtype_size(dt)) return S4C_ERR_ALIGN;
-    const LpParams p = {logits, row_stride, tokens, nullptr, nullptr, nullptr, 0, 0, V, top, kLog2E / temperature, temperature / kLog2E, logprob, entropy, top_token, top_logprob, status};
+    const LpParams p = {logits, row_stride, tokens, nullptr, nullptr, nullptr, 0, 0, V, top, kLog2E / temperature, temperature / kLog2E, 1.4426950408889634 / temperature, logprob, entropy, top_token, top_logprob, status};
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     return dt == S4C_F32 ? lp_launch<float>(p, R, stream) : lp_launch<__nv_bfloat16>(p, R, stream);
 }
@@ -540,7 +541,7 @@ extern "C" s4c_status s4c_tree_logprobs(const void* logits, const int32_t* token
     if (dt != S4C_F32 && dt != S4C_BF16) return S4C_ERR_DTYPE;
     if (top > kLpMaxTop) return S4C_ERR_UNSUPPORTED;
     if (reinterpret_cast<uintptr_t>(logits) % dtype_size(dt)) return S4C_ERR_ALIGN;
-    const LpParams p = {logits, V, tokens, path, accept_len, next_token, max_depth + 1, T, V, top, kLog2E / temperature, temperature / kLog2E, logprob, entropy, top_token, top_logprob, status};
+    const LpParams p = {logits, V, tokens, path, accept_len, next_token, max_depth + 1, T, V, top, kLog2E / temperature, temperature / kLog2E, 1.4426950408889634 / temperature, logprob, entropy, top_token, top_logprob, status};
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     return dt == S4C_F32 ? lp_launch<float>(p, (long long)B * (max_depth + 1), stream) : lp_launch<__nv_bfloat16>(p, (long long)B * (max_depth + 1), stream);
 }
