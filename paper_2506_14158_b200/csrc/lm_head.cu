@@ -49,6 +49,13 @@ struct LmCfg {
     static constexpr int kSmemBytes = 1024 + kRingBytes + kBars * 8 + 16;
 };
 
+// y = (x - m) log2(e) / temperature as (x pre - m pre) by: pre is 1, and 1/4 from temperature 1e30 on, where the difference of two finite logits may leave
+// float32 and log2(e) / temperature may be subnormal (flushed to 0, whose product with a masked logit is no -Inf) while y matters.
+struct LmScale {
+    float pre, by;
+    __device__ __forceinline__ float apart(float x, float m_pre) const { return fmaf(x, pre, -m_pre) * by; }
+};
+
 struct LmParams {
     int rows;        // rows of this launch (<= 256), starting at row0 of the hidden states
     int row0;
@@ -61,42 +68,42 @@ struct LmParams {
     int32_t* part_t; // [256][kLmMaxParts][KT] and their tokens
     int32_t* gave_up; // [kLmMaxParts]: 1 where the CTA gave up a wait
     // of s4c_lm_head_logprobs alone
-    float scale;      // log2(e) / temperature
+    LmScale scale;
     const int32_t* tokens;  // [R] or NULL
     float4* part_s;   // [256][kLmMaxParts] per row the CTAs' maximum m, sum of 2^y and sum of 2^y y, y = (x - m) scale
     float* given;     // [256] the logit of the row's token
 };
 
-// A row's running softmax statistics: the maximum so far, S = sum 2^y and E = sum 2^y y with y = (x - m) scale.
+// A row's running softmax statistics: the maximum so far, S = sum 2^y and E = sum 2^y y with y as above.
 struct LmStats {
     float m, S, E;
 };
-// Moves statistics to a greater maximum: y becomes y + d with d = (m - m_new) scale <= 0, so S -> S 2^d, E -> (E + S d) 2^d.
-__device__ __forceinline__ void lm_stats_raise(LmStats& s, float m_new, float scale) {
+// Moves statistics to a greater maximum: y becomes y + d with d = y(m) against m_new <= 0, so S -> S 2^d, E -> (E + S d) 2^d.
+__device__ __forceinline__ void lm_stats_raise(LmStats& s, float m_new, const LmScale& scale) {
     if (s.m > -INFINITY) {
-        const float d = fmaxf((s.m - m_new) * scale, -200.0f), f = rows::exp2_fast(d);
+        const float d = fmaxf(scale.apart(s.m, m_new * scale.pre), -200.0f), f = rows::exp2_fast(d);
         s.E = (s.E + s.S * d) * f, s.S *= f;
     }
     s.m = m_new;
 }
 // Takes a run of 32 logits in.  A NaN in the run makes S a NaN (maxima pass it over), a +Inf likewise (Inf - Inf).
-__device__ __forceinline__ void lm_stats_run(LmStats& s, const uint32_t (&r)[32], float scale) {
+__device__ __forceinline__ void lm_stats_run(LmStats& s, const uint32_t (&r)[32], const LmScale& scale) {
     float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
     for (int j = 0; j < 32; ++j) mx[j & 3] = fmaxf(mx[j & 3], __uint_as_float(r[j]));
     const float m = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
     if (m > s.m) lm_stats_raise(s, m, scale);
     float S[4] = {0, 0, 0, 0}, E[4] = {0, 0, 0, 0};
-    const float ref = s.m > -INFINITY ? s.m : 0.0f;  // (nothing but -Inf so far: terms of 0, not of NaN)
+    const float ref = s.m > -INFINITY ? s.m * scale.pre : 0.0f;  // (nothing but -Inf so far: terms of 0, not of NaN)
 #pragma unroll
     for (int j = 0; j < 32; ++j) {
-        const float d = (__uint_as_float(r[j]) - ref) * scale, y = d < -200.0f ? -200.0f : d;  // (keeps a NaN; 2^-200 is 0, and -Inf times 0 would not be)
+        const float d = scale.apart(__uint_as_float(r[j]), ref), y = d < -200.0f ? -200.0f : d;  // (keeps a NaN; 2^-200 is 0, and -Inf times 0 would not be)
         const float e = rows::exp2_fast(y);
         S[j & 3] += e, E[j & 3] += e * y;
     }
     s.S += (S[0] + S[1]) + (S[2] + S[3]), s.E += (E[0] + E[1]) + (E[2] + E[3]);
 }
-__device__ __forceinline__ void lm_stats_join(LmStats& a, LmStats b, float scale) {
+__device__ __forceinline__ void lm_stats_join(LmStats& a, LmStats b, const LmScale& scale) {
     if (b.m > a.m)
         lm_stats_raise(a, b.m, scale);
     else if (a.m > b.m)
@@ -125,13 +132,13 @@ __device__ __forceinline__ void lm_last_rows(const LmParams& prm, const float* s
 #pragma unroll
         for (int i = 0; i < kMost; ++i) m = fmaxf(m, v[i]);
         m = rows::warp_max(m);
-        const float ref = m > -INFINITY ? m : 0.0f;
+        const float ref = m > -INFINITY ? m * prm.scale.pre : 0.0f;
         LmStats st = {ps.x, ps.y, ps.z};
         if (m > st.m) lm_stats_raise(st, m, prm.scale);
         float S = st.S, E = st.E;
 #pragma unroll
         for (int i = 0; i < kMost; ++i) {
-            const float d = (v[i] - ref) * prm.scale, y = d < -200.0f ? -200.0f : d, e = rows::exp2_fast(y);
+            const float d = prm.scale.apart(v[i], ref), y = d < -200.0f ? -200.0f : d, e = rows::exp2_fast(y);
             S += e, E += e * y;
         }
         S = rows::warp_sum(S), E = rows::warp_sum(E);
@@ -558,7 +565,7 @@ struct LmLogprobs {
     const float* given;
     const int32_t* tokens;  // the launch's rows, or NULL
     int n_parts, V, k;
-    float scale;
+    LmScale scale;
     float* logprob;         // [rows] or NULL
     float* entropy;         // [rows] or NULL
     int32_t* token;         // [rows, k]
@@ -637,7 +644,7 @@ lm_head_logprobs_merge_kernel(const LmLogprobs p) {
     const int flags = (dead ? S4C_SEQ_TIMEOUT : 0) | (!skip && !sound ? S4C_SEQ_NONFINITE : 0);
     const bool fine = !skip && !flags;
     const float ln_s = sound ? rows::ln_series(st.S) : 0.0f;
-    const double ln_scale = (double)p.scale * rows::kLn2;
+    const double ln_scale = (double)p.scale.by * p.scale.pre * rows::kLn2;
     auto logprob = [&](float x) { return (float)(((double)x - st.m) * ln_scale - ln_s); };
     if (tid == 0) {
         if (p.logprob) p.logprob[r] = skip ? 0.0f : fine && in_range ? logprob(p.given[r]) : NAN;
@@ -915,7 +922,8 @@ extern "C" s4c_status s4c_lm_head_logprobs(const void* hidden, const void* weigh
     LmParams prm = {};
     if (!workspace || workspace_bytes < lm_lp_layout(top, nullptr, nullptr) || !aligned256(workspace)) return S4C_ERR_WORKSPACE;
     lm_lp_layout(top, static_cast<char*>(workspace), &prm);
-    prm.scale = rows::kLog2E / temperature, prm.tokens = tokens;
+    prm.scale = temperature < 1e30f ? LmScale{1.0f, rows::kLog2E / temperature} : LmScale{0.25f, (float)(4.0 * rows::kLog2E / temperature)};
+    prm.tokens = tokens;
     LmLogprobs lp = {};
     lp.part_s = prm.part_s, lp.given = prm.given, lp.tokens = tokens, lp.V = V, lp.scale = prm.scale;
     lp.logprob = logprob, lp.entropy = entropy, lp.choice = choice;

@@ -62,3 +62,29 @@ def test_a_walk_at_the_ends_of_the_temperatures():
         tau = float(np.float32(tau))
         got = s4c.tree_logprobs(x.cuda(), d(tokens), d(path), d(accept_len), d(next_token), tau, 4)
         check({k: v[0] for k, v in got.items()}, oracle.token_logprobs(x[0].double().numpy(), emitted, tau, 4), V, 4)
+
+
+@pytest.mark.parametrize("R,V", [(3, 1), (26, 1000), (26, 4101), (130, 4101)])
+def test_the_lm_head_at_the_ends_of_the_temperatures(R, V):
+    """States of one 1 each, so that logits[r, v] = weight[v, r % 64] exactly: the columns' values are those of the rows above."""
+    from paper_2506_14158_b200 import s4c
+
+    H = 64
+    h = torch.zeros(R, H, dtype=torch.bfloat16)
+    h[torch.arange(R), torch.arange(R) % H] = 1
+    kinds = rows(V, "bf16")[[0, 3, 4, 6, 8]]  # (infinities and NaN of one column would meet the zeros of every state)
+    w = torch.from_numpy(kinds[np.arange(H) % len(kinds)].T.copy()).to(torch.bfloat16)
+    masked = np.isneginf(w.double().numpy())
+    w[torch.from_numpy(masked)] = 0.0
+    h[:, H - 1], w[:, H - 1] = 1, 0.0
+    if V > 2:
+        w[V // 2:V // 2 + V // 8, H - 1] = -np.inf  # masked for every row: the maximum is elsewhere
+    x = w[:, :H - 1].double().numpy()[:, np.arange(R) % H % (H - 1)].T.copy()
+    x[np.arange(R) % H == H - 1] = 0.0
+    if V > 2:
+        x[:, V // 2:V // 2 + V // 8] = -np.inf
+    tok = (np.arange(R) * 7 % V).astype(np.int32)
+    for tau in TEMPERATURES:
+        tau = float(np.float32(tau))
+        got = s4c.lm_head_logprobs(h.cuda(), w.cuda(), torch.from_numpy(tok).cuda(), tau, 5)
+        check(got, oracle.token_logprobs(x, tok, tau, 5), V, 5)
