@@ -383,6 +383,9 @@ s4c_status s4c_lm_head_logits(const void* hidden, const void* weight, int R, int
  *                      product is formed for rows that are not asked for too; status also S4C_SEQ_TIMEOUT (as a NONFINITE row).
  *                      choice [R] int32 or NULL: every row's token as s4c_lm_head_greedy writes it (whatever tokens[r] and the
  *                      flags say), for the greedy walk behind (s4c_tree_accept_tokens).
+ * s4c_lm_head_greedy_logprobs   the same call with what else s4c_lm_head_greedy writes, for programs that go on from the choice:
+ *                      max_logit [R] f32 or NULL, and call_status, one int32 or NULL: set to 0 and OR-ed with S4C_SEQ_TIMEOUT if
+ *                      a wait inside the kernel ran out.
  * ------------------------------------------------------------------------------------------ */
 #define S4C_MAX_LOGITS_ROWS (1 << 27)
 #define S4C_MAX_LOGITS_COLUMNS (1 << 30)
@@ -402,6 +405,11 @@ s4c_status s4c_lm_head_logprobs(const void* hidden, const void* weight, const in
                                 float temperature, int top, float* logprob, float* entropy, int32_t* top_token,
                                 float* top_logprob, int32_t* choice, int32_t* status, void* workspace,
                                 size_t workspace_bytes, s4c_stream_t stream);
+
+s4c_status s4c_lm_head_greedy_logprobs(const void* hidden, const void* weight, const int32_t* tokens, int R, int V, int H,
+                                       float temperature, int top, float* logprob, float* entropy, int32_t* top_token,
+                                       float* top_logprob, int32_t* choice, float* max_logit, int32_t* status,
+                                       int32_t* call_status, void* workspace, size_t workspace_bytes, s4c_stream_t stream);
 
 /* ------------------------------------------------------------------------------------------
  * s4c_distill_topk, s4c_distill_topk_backward -- the drafter's training signal at its heads' logits (Section 3.1.2: cross

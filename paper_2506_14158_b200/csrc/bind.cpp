@@ -475,11 +475,11 @@ PyObject* tree_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// lm_head_logprobs(hidden, weight, tokens, temperature, top, logprob, entropy, top_token, top_logprob, status, choice, workspace, stream)
-// -> (rc, outputs).  A workspace that is None is the call's own: calls on several streams, and captured ones, share nothing.
+// lm_head_logprobs(hidden, weight, tokens, temperature, top, logprob, entropy, top_token, top_logprob, status, choice, workspace, stream, max_logit,
+// call_status) -> (rc, outputs).  A workspace that is None is the call's own: calls on several streams, and captured ones, share nothing.
 PyObject* lm_head_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
-        count(n, 13);
+        count(n, 15);
         const at::Tensor &h = tensor(a[0], "hidden"), &w = tensor(a[1], "weight");
         if (h.dim() != 2 || w.dim() != 2) {
             PyErr_SetString(PyExc_ValueError, "hidden must be [R,H] and weight [V,H]");
@@ -492,6 +492,8 @@ PyObject* lm_head_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const float temperature = to_real(a[3]);
         const int top = to_integer(a[4]);
         int32_t* choice = static_cast<int32_t*>(beside(a[10], h, {R}, at::kInt, "choice"));
+        float* max_logit = static_cast<float*>(beside(a[13], h, {R}, at::kFloat, "max_logit"));
+        int32_t* call_status = static_cast<int32_t*>(beside(a[14], h, {1}, at::kInt, "call_status"));
         LogprobOutputs out(a + 5, h, {R}, top, a[2] != Py_None);
         try {
             const On on(h, a[12]);
@@ -506,8 +508,8 @@ PyObject* lm_head_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
             void* p = own.defined() ? own.data_ptr() : scratch.p;
             const size_t bytes = own.defined() ? (size_t)own.nbytes() : scratch.bytes;
             return out.result(unlocked([&] {
-                return s4c_lm_head_logprobs(hidden, weight, tokens, R, V, H, temperature, top, out.logprob, out.entropy, out.top_token, out.top_logprob,
-                                            choice, out.status, p, bytes, on.stream);
+                return s4c_lm_head_greedy_logprobs(hidden, weight, tokens, R, V, H, temperature, top, out.logprob, out.entropy, out.top_token,
+                                                   out.top_logprob, choice, max_logit, out.status, call_status, p, bytes, on.stream);
             }));
         } catch (...) {
             out.release();

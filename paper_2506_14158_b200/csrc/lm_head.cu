@@ -571,6 +571,9 @@ struct LmLogprobs {
     int32_t* token;         // [rows, k]
     float* top_logprob;
     int32_t* choice;        // [rows] or NULL: the greedy choice
+    float* max_logit;       // [rows] or NULL: its logit
+    int32_t* call_status;   // one word or NULL: what s4c_lm_head_greedy's status says
+    int first;              // the call's first launch
     int32_t* status;        // [rows] or NULL
 };
 template <int KT>
@@ -651,17 +654,21 @@ lm_head_logprobs_merge_kernel(const LmLogprobs p) {
         if (p.entropy) p.entropy[r] = skip ? 0.0f : fine ? ln_s - __fdividef(st.E, st.S) * (float)rows::kLn2 : NAN;
         if (p.status) p.status[r] = flags | (!skip && p.tokens && !in_range ? S4C_SEQ_TOKEN_RANGE : 0);
         if (p.choice && found == 0) p.choice[r] = -1;
+        if (p.max_logit && found == 0) p.max_logit[r] = -INFINITY;
+        if (p.call_status && r == 0) *p.call_status = (p.first ? 0 : *p.call_status) | (dead ? S4C_SEQ_TIMEOUT : 0);
     }
     for (int i = tid; i < found; i += kLmMaxParts) {
         const uint64_t key = candidate[i];
         int place = 0;
         for (int j = 0; j < found; ++j) place += candidate[j] > key;
         const int token = (int)(0xffffffffu - (uint32_t)key);
+        const uint32_t b = (uint32_t)(key >> 32);
+        const float x = __uint_as_float(b ^ ((b >> 31) ? 0x80000000u : 0xffffffffu));
         if (place == 0 && p.choice) p.choice[r] = token;
+        if (place == 0 && p.max_logit) p.max_logit[r] = x;
         if (place < p.k && fine) {
-            const uint32_t b = (uint32_t)(key >> 32);
             p.token[(size_t)r * p.k + place] = token;
-            p.top_logprob[(size_t)r * p.k + place] = logprob(__uint_as_float(b ^ ((b >> 31) ? 0x80000000u : 0xffffffffu)));
+            p.top_logprob[(size_t)r * p.k + place] = logprob(x);
         }
     }
     for (int j = (fine ? found : 0) + tid; j < p.k; j += kLmMaxParts) p.token[(size_t)r * p.k + j] = -1, p.top_logprob[(size_t)r * p.k + j] = -INFINITY;
@@ -841,6 +848,7 @@ static s4c_status lm_groups(const void* hidden, const void* weight, int R, int V
     const int32_t* tokens = lp.tokens;
     float *logprob = lp.logprob, *entropy = lp.entropy;
     int32_t* choice = lp.choice;
+    float* max_logit = lp.max_logit;
     const int sms = std::min(lm_sm_count(), kLmMaxParts);
     for (int row0 = 0; row0 < R; row0 += kLmRowsPerLaunch) {
         prm.rows = std::min(kLmRowsPerLaunch, R - row0), prm.row0 = row0, prm.V = V, prm.k_steps = H / kLmBK;
@@ -870,7 +878,8 @@ static s4c_status lm_groups(const void* hidden, const void* weight, int R, int V
         if (LP) {
             lp.tokens = tokens ? tokens + row0 : nullptr;
             lp.logprob = logprob ? logprob + row0 : nullptr, lp.entropy = entropy ? entropy + row0 : nullptr;
-            lp.choice = choice ? choice + row0 : nullptr;
+            lp.choice = choice ? choice + row0 : nullptr, lp.max_logit = max_logit ? max_logit + row0 : nullptr;
+            lp.first = row0 == 0;
         }
         const s4c_status st = kt == 1   ? lm_run<1, LP>(map_h, map_w, prm, grid, k, tok, lgt, sts, lp, stream)
                               : kt == 4 ? lm_run<4, LP>(map_h, map_w, prm, grid, k, tok, lgt, sts, lp, stream)
@@ -908,9 +917,10 @@ extern "C" size_t s4c_lm_head_logprobs_workspace_bytes(int R, int V, int H, int 
     return s4c::lm_lp_layout(top, nullptr, nullptr);
 }
 
-extern "C" s4c_status s4c_lm_head_logprobs(const void* hidden, const void* weight, const int32_t* tokens, int R, int V, int H, float temperature,
-                                           int top, float* logprob, float* entropy, int32_t* top_token, float* top_logprob, int32_t* choice,
-                                           int32_t* status, void* workspace, size_t workspace_bytes, s4c_stream_t stream_) {
+extern "C" s4c_status s4c_lm_head_greedy_logprobs(const void* hidden, const void* weight, const int32_t* tokens, int R, int V, int H, float temperature,
+                                                  int top, float* logprob, float* entropy, int32_t* top_token, float* top_logprob, int32_t* choice,
+                                                  float* max_logit, int32_t* status, int32_t* call_status, void* workspace, size_t workspace_bytes,
+                                                  s4c_stream_t stream_) {
     using namespace s4c;
     if (R == 0 && V >= 1) return S4C_OK;
     if (!hidden || !weight || (logprob && !tokens) || (top > 0 && (!top_token || !top_logprob))) return S4C_ERR_NULL;
@@ -926,8 +936,15 @@ extern "C" s4c_status s4c_lm_head_logprobs(const void* hidden, const void* weigh
     prm.tokens = tokens;
     LmLogprobs lp = {};
     lp.part_s = prm.part_s, lp.given = prm.given, lp.tokens = tokens, lp.V = V, lp.scale = prm.scale;
-    lp.logprob = logprob, lp.entropy = entropy, lp.choice = choice;
+    lp.logprob = logprob, lp.entropy = entropy, lp.choice = choice, lp.max_logit = max_logit, lp.call_status = call_status;
     return lm_groups<true>(hidden, weight, R, V, H, top, lm_kt(top), top_token, top_logprob, status, prm, lp, static_cast<cudaStream_t>(stream_));
+}
+
+extern "C" s4c_status s4c_lm_head_logprobs(const void* hidden, const void* weight, const int32_t* tokens, int R, int V, int H, float temperature,
+                                           int top, float* logprob, float* entropy, int32_t* top_token, float* top_logprob, int32_t* choice,
+                                           int32_t* status, void* workspace, size_t workspace_bytes, s4c_stream_t stream) {
+    return s4c_lm_head_greedy_logprobs(hidden, weight, tokens, R, V, H, temperature, top, logprob, entropy, top_token, top_logprob, choice, nullptr, status,
+                                       nullptr, workspace, workspace_bytes, stream);
 }
 
 extern "C" size_t s4c_lm_head_greedy_workspace_bytes(int R, int V, int H) { return s4c_lm_head_topk_workspace_bytes(R, V, H, 1); }

@@ -29,7 +29,7 @@ EXPORTS = ["s4c_version", "s4c_status_string", "s4c_tree_attention_workspace_byt
            "s4c_tree_accept_filtered", "s4c_lm_head_greedy_workspace_bytes", "s4c_lm_head_greedy", "s4c_tree_accept_tokens",
            "s4c_qkv_rope_workspace_bytes", "s4c_qkv_rope", "s4c_qkv_rope_at", "s4c_qkv_rope_same_tree", "s4c_lm_head_topk_workspace_bytes", "s4c_lm_head_topk",
            "s4c_tree_build_topk", "s4c_draft_level", "s4c_lm_head_logits_workspace_bytes", "s4c_lm_head_logits", "s4c_linear_workspace_bytes", "s4c_linear", "s4c_linear_rmsnorm", "s4c_rmsnorm", "s4c_embed_gather",
-           "s4c_token_logprobs", "s4c_tree_logprobs", "s4c_lm_head_logprobs_workspace_bytes", "s4c_lm_head_logprobs", "s4c_distill_topk",
+           "s4c_token_logprobs", "s4c_tree_logprobs", "s4c_lm_head_logprobs_workspace_bytes", "s4c_lm_head_logprobs", "s4c_lm_head_greedy_logprobs", "s4c_distill_topk",
            "s4c_distill_topk_backward"]
 NOALLOC_SCRATCH_BYTES = 1 << 20
 
@@ -661,11 +661,12 @@ def lm_head_logprobs_workspace_bytes(R, V, H, top) -> int:
 
 
 def lm_head_logprobs(hidden, weight, tokens=None, temperature: float = 1.0, top: int = 0, logprob=None, entropy=None, top_token=None,
-                     top_logprob=None, status=None, choice=None, workspace=None, stream=None):
+                     top_logprob=None, status=None, choice=None, workspace=None, stream=None, max_logit=None, call_status=None):
     """s4c_lm_head_logprobs: :func:`token_logprobs` of hidden @ weight^T (bf16 in, f32 sums) without logits in memory; top <= 8.
-    ``choice`` [R] int32 receives every row's greedy choice (:func:`lm_head_greedy`'s token)."""
+    ``choice`` [R] int32, ``max_logit`` [R] and ``call_status`` [1] int32, where given, receive what :func:`lm_head_greedy` writes as token,
+    max_logit and status (s4c_lm_head_greedy_logprobs)."""
     rc, out = _bind.lm_head_logprobs(hidden, weight, tokens, temperature, top, logprob, entropy, top_token, top_logprob, status, choice, workspace,
-                                     stream)
+                                     stream, max_logit, call_status)
     if rc:
         raise S4CError("s4c_lm_head_logprobs", rc)
     return dict(zip(_LOGPROB_OUTPUTS, out))

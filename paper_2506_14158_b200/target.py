@@ -12,7 +12,7 @@ chat models):
         x_{l+1} = h + g Wd^T,       a_{l+1} = rmsnorm(x_{l+1})   s4c_linear_rmsnorm    (the next layer's norm, or the final norm)
     greedy (Section 4.1):
     target token per node = Argmax(LM_head(a_n))                 s4c_lm_head_greedy    (no [B,T,V] logits in memory; with log
-                                                                 probabilities asked for: s4c_lm_head_logprobs, the same choice)
+                                                                 probabilities asked for: s4c_lm_head_greedy_logprobs, the same choice)
     longest accepted path, next token                            s4c_tree_accept_tokens
     speculative sampling (Eq. 11-12, temperature > 0):
     logits = LM_head(a_n) as float32 [B,T,V]                     s4c_lm_head_logits
@@ -175,7 +175,7 @@ class TargetVerify:
                 s4c.lm_head_greedy(self.a[last], w.lm_head, self.target_token, self.max_logit, self.status_head, self.ws_head)
             else:
                 s4c.lm_head_logprobs(self.a[last], w.lm_head, None, 1.0, self.top_logprobs, choice=self.target_token, workspace=self.ws_logprobs,
-                                     **self.node_logprobs)
+                                     max_logit=self.max_logit, call_status=self.status_head, **self.node_logprobs)
             s4c.tree_accept_tokens(self.target_token.view(B, T), tokens, parent, self.V, n_nodes, self.max_depth, self.accept_len,
                                    self.path, self.next_token, self.status_accept)
         if compact:
