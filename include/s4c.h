@@ -649,6 +649,18 @@ s4c_status s4c_selftest_attention_timeout(const void* q, const void* k_cache, co
                                           int Hq, int Hkv, int d, int C, int max_cache_len, int withhold_tile,
                                           int limit_us, int32_t* status, s4c_stream_t stream);
 
+/* ------------------------------------------------------------------------------------------
+ * s4c_selftest_lm_head_timeout -- the same check for the LM head: s4c_lm_head_greedy_logprobs without tokens at temperature 1,
+ * in which the hidden states of vocabulary tile `withhold_tile` (0-based; 64 to 256 tokens each) are never requested and the
+ * wait for them runs out after its usual 200 ms.  Afterwards call_status and every row's status hold S4C_SEQ_TIMEOUT, entropy
+ * is NaN, the alternatives are -1 / -Inf, choice is the best token of what the other CTAs (and part of that one) computed and
+ * max_logit its logit (-1 and -Inf where nothing was), and the next call on the stream works normally.
+ * ------------------------------------------------------------------------------------------ */
+s4c_status s4c_selftest_lm_head_timeout(const void* hidden, const void* weight, int R, int V, int H, int top, float* entropy,
+                                        int32_t* top_token, float* top_logprob, int32_t* choice, float* max_logit,
+                                        int32_t* status, int32_t* call_status, void* workspace, size_t workspace_bytes,
+                                        int withhold_tile, s4c_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -67,6 +67,7 @@ struct LmParams {
     float* part_v;   // [256][kLmMaxParts][KT] per row the CTAs' best logits, best first
     int32_t* part_t; // [256][kLmMaxParts][KT] and their tokens
     int32_t* gave_up; // [kLmMaxParts]: 1 where the CTA gave up a wait
+    int withhold_tile; // -1; the self-test names one tile for which no hidden states are requested
     // of s4c_lm_head_logprobs alone
     LmScale scale;
     const int32_t* tokens;  // [R] or NULL
@@ -232,6 +233,7 @@ lm_head_greedy_kernel(const __grid_constant__ CUtensorMap map_h, const __grid_co
             bool ok = true;
             for (int tile = blockIdx.x; tile < n_tiles && ok; tile += gridDim.x) {
                 const int row = tile * bn;
+                if (states && tile == prm.withhold_tile) break;
                 for (int ks = 0; ks < prm.k_steps; ++ks, ++fill) {
                     ok = mbar_wait(EMPTY(s), ph, dead);
                     if (!ok) break;
@@ -403,7 +405,18 @@ lm_head_greedy_kernel(const __grid_constant__ CUtensorMap map_h, const __grid_co
                 prior_s[grp * kLmBM + q * 32 + lane] = make_float4(stats[0].m, stats[0].S, stats[0].E, 0.0f);
             }
             named_bar_sync(1, 128 * kLmEpiGroups);
-            if (fine) lm_last_rows<KT>(prm, spread, pitch, last_col, min(bn, prm.V - last_col), prior_v, prior_t, prior_s, warp - kLmRoleWarps, lane);
+            const int row = q * 32 + lane;
+            if (fine) {
+                lm_last_rows<KT>(prm, spread, pitch, last_col, min(bn, prm.V - last_col), prior_v, prior_t, prior_s, warp - kLmRoleWarps, lane);
+            } else if (grp == 0 && row < prm.rows) {
+                // (a CTA that gave up a wait: the call is flagged, but the merge and the choice behind it read lists of this call all the same)
+                prm.part_s[(size_t)row * kLmMaxParts + blockIdx.x] = make_float4(stats[0].m, stats[0].S, stats[0].E, 0.0f);
+#pragma unroll
+                for (int j = 0; j < KT; ++j) {
+                    prm.part_v[((size_t)row * kLmMaxParts + blockIdx.x) * KT + j] = best_v[0][j];
+                    prm.part_t[((size_t)row * kLmMaxParts + blockIdx.x) * KT + j] = best_t[0][j];
+                }
+            }
         } else {
         // The groups' lists of a row become one: the second group leaves its own in shared memory (in the ring, which nothing uses
         // any more once every group is through the last tile), the first one takes its entries in.  (A group that gave up a wait
@@ -906,6 +919,7 @@ extern "C" s4c_status s4c_lm_head_topk(const void* hidden, const void* weight, i
     if (!aligned16(hidden) || !aligned16(weight)) return S4C_ERR_ALIGN;
     if (R == 0) return S4C_OK;
     LmParams prm = {};
+    prm.withhold_tile = -1;
     const size_t need = lm_ws_layout(k, nullptr, nullptr, nullptr, nullptr);
     if (!workspace || workspace_bytes < need || !aligned256(workspace)) return S4C_ERR_WORKSPACE;
     lm_ws_layout(k, static_cast<char*>(workspace), &prm.part_v, &prm.part_t, &prm.gave_up);
@@ -917,11 +931,10 @@ extern "C" size_t s4c_lm_head_logprobs_workspace_bytes(int R, int V, int H, int 
     return s4c::lm_lp_layout(top, nullptr, nullptr);
 }
 
-extern "C" s4c_status s4c_lm_head_greedy_logprobs(const void* hidden, const void* weight, const int32_t* tokens, int R, int V, int H, float temperature,
-                                                  int top, float* logprob, float* entropy, int32_t* top_token, float* top_logprob, int32_t* choice,
-                                                  float* max_logit, int32_t* status, int32_t* call_status, void* workspace, size_t workspace_bytes,
-                                                  s4c_stream_t stream_) {
-    using namespace s4c;
+namespace s4c {
+static s4c_status lm_logprobs(const void* hidden, const void* weight, const int32_t* tokens, int R, int V, int H, float temperature, int top, float* logprob,
+                              float* entropy, int32_t* top_token, float* top_logprob, int32_t* choice, float* max_logit, int32_t* status,
+                              int32_t* call_status, void* workspace, size_t workspace_bytes, int withhold_tile, s4c_stream_t stream_) {
     if (R == 0 && V >= 1) return S4C_OK;
     if (!hidden || !weight || (logprob && !tokens) || (top > 0 && (!top_token || !top_logprob))) return S4C_ERR_NULL;
     if (R < 0 || V < 1 || H < kLmBK || H % kLmBK != 0 || top < 0 || !(temperature > 0.0f) || !(temperature < INFINITY) ||
@@ -933,11 +946,30 @@ extern "C" s4c_status s4c_lm_head_greedy_logprobs(const void* hidden, const void
     if (!workspace || workspace_bytes < lm_lp_layout(top, nullptr, nullptr) || !aligned256(workspace)) return S4C_ERR_WORKSPACE;
     lm_lp_layout(top, static_cast<char*>(workspace), &prm);
     prm.scale = temperature < 1e30f ? LmScale{1.0f, rows::kLog2E / temperature} : LmScale{0.25f, (float)(4.0 * rows::kLog2E / temperature)};
-    prm.tokens = tokens;
+    prm.tokens = tokens, prm.withhold_tile = withhold_tile;
     LmLogprobs lp = {};
     lp.part_s = prm.part_s, lp.given = prm.given, lp.tokens = tokens, lp.V = V, lp.scale = prm.scale;
     lp.logprob = logprob, lp.entropy = entropy, lp.choice = choice, lp.max_logit = max_logit, lp.call_status = call_status;
     return lm_groups<true>(hidden, weight, R, V, H, top, lm_kt(top), top_token, top_logprob, status, prm, lp, static_cast<cudaStream_t>(stream_));
+}
+}  // namespace s4c
+
+extern "C" s4c_status s4c_lm_head_greedy_logprobs(const void* hidden, const void* weight, const int32_t* tokens, int R, int V, int H, float temperature,
+                                                  int top, float* logprob, float* entropy, int32_t* top_token, float* top_logprob, int32_t* choice,
+                                                  float* max_logit, int32_t* status, int32_t* call_status, void* workspace, size_t workspace_bytes,
+                                                  s4c_stream_t stream) {
+    return s4c::lm_logprobs(hidden, weight, tokens, R, V, H, temperature, top, logprob, entropy, top_token, top_logprob, choice, max_logit, status, call_status,
+                            workspace, workspace_bytes, -1, stream);
+}
+
+// The bounded waits of the LM head, exercised: no hidden states are requested for vocabulary tile `withhold_tile` (and what follows it in its CTA), the
+// products' wait for them runs out after the usual limit, every role of that CTA leaves its loop, and the call returns normally, flagged.
+extern "C" s4c_status s4c_selftest_lm_head_timeout(const void* hidden, const void* weight, int R, int V, int H, int top, float* entropy, int32_t* top_token,
+                                                   float* top_logprob, int32_t* choice, float* max_logit, int32_t* status, int32_t* call_status,
+                                                   void* workspace, size_t workspace_bytes, int withhold_tile, s4c_stream_t stream) {
+    if (withhold_tile < 0) return S4C_ERR_SHAPE;
+    return s4c::lm_logprobs(hidden, weight, nullptr, R, V, H, 1.0f, top, nullptr, entropy, top_token, top_logprob, choice, max_logit, status, call_status,
+                            workspace, workspace_bytes, withhold_tile, stream);
 }
 
 extern "C" s4c_status s4c_lm_head_logprobs(const void* hidden, const void* weight, const int32_t* tokens, int R, int V, int H, float temperature,

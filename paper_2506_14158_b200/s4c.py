@@ -24,7 +24,7 @@ STATUS_NAMES = ["OK", "ERR_NULL", "ERR_SHAPE", "ERR_DTYPE", "ERR_ALIGN", "ERR_WO
 
 EXPORTS = ["s4c_version", "s4c_status_string", "s4c_tree_attention_workspace_bytes", "s4c_tree_attention", "s4c_tree_attention_rows",
            "s4c_tree_accept_workspace_bytes", "s4c_tree_accept", "s4c_tree_accept_noalloc", "s4c_kv_compact",
-           "s4c_launch_floor", "s4c_selftest_attention_timeout", "s4c_tree_build_workspace_bytes", "s4c_tree_build",
+           "s4c_launch_floor", "s4c_selftest_attention_timeout", "s4c_selftest_lm_head_timeout", "s4c_tree_build_workspace_bytes", "s4c_tree_build",
            "s4c_tree_attention_paged", "s4c_kv_compact_paged", "s4c_tree_accept_filtered_workspace_bytes",
            "s4c_tree_accept_filtered", "s4c_lm_head_greedy_workspace_bytes", "s4c_lm_head_greedy", "s4c_tree_accept_tokens",
            "s4c_qkv_rope_workspace_bytes", "s4c_qkv_rope", "s4c_qkv_rope_at", "s4c_qkv_rope_same_tree", "s4c_lm_head_topk_workspace_bytes", "s4c_lm_head_topk",
@@ -104,6 +104,8 @@ def _load() -> ctypes.CDLL:
     lib.s4c_embed_gather.argtypes = [vp, i32p, i, i, i, vp, vp]
     lib.s4c_lm_head_logprobs_workspace_bytes.restype = sz
     lib.s4c_lm_head_logprobs_workspace_bytes.argtypes = [i, i, i, i]
+    lib.s4c_selftest_lm_head_timeout.restype = i
+    lib.s4c_selftest_lm_head_timeout.argtypes = [vp, vp, i, i, i, i, vp, i32p, vp, i32p, vp, i32p, i32p, vp, sz, i, vp]
     lib.s4c_launch_floor.restype = i
     lib.s4c_launch_floor.argtypes = [i, i, i, i, i, i, i, i32p, i32p, vp]
     return lib
@@ -670,6 +672,19 @@ def lm_head_logprobs(hidden, weight, tokens=None, temperature: float = 1.0, top:
     if rc:
         raise S4CError("s4c_lm_head_logprobs", rc)
     return dict(zip(_LOGPROB_OUTPUTS, out))
+
+
+def selftest_lm_head_timeout(hidden, weight, entropy, top_token, top_logprob, choice, max_logit, status, call_status, workspace, withhold_tile: int,
+                             stream=None):
+    """s4c_selftest_lm_head_timeout: the LM head with log probabilities, the hidden states of one vocabulary tile withheld."""
+    f32, i32 = torch.float32, torch.int32
+    rc = _lib.s4c_selftest_lm_head_timeout(
+        _dev(hidden, torch.bfloat16, "hidden"), _dev(weight, torch.bfloat16, "weight"), hidden.shape[0], weight.shape[0], hidden.shape[1],
+        top_token.shape[1], _dev(entropy, f32, "entropy"), _dev(top_token, i32, "top_token"), _dev(top_logprob, f32, "top_logprob"),
+        _dev(choice, i32, "choice"), _dev(max_logit, f32, "max_logit"), _dev(status, i32, "status"), _dev(call_status, i32, "call_status"),
+        _dev(workspace, torch.uint8, "workspace"), workspace.numel(), int(withhold_tile), _stream(stream))
+    if rc:
+        raise S4CError("s4c_selftest_lm_head_timeout", rc)
 
 
 def distill_topk(logits, teacher_token=None, teacher_logit=None, labels=None, temperature: float = 1.0, teacher_weight: float = 1.0,
