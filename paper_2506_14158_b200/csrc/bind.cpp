@@ -344,6 +344,13 @@ void* beside(PyObject* o, const at::Tensor& anchor, at::IntArrayRef shape, at::S
     }
     return p;
 }
+// A tensor that a call writes counts as changed, as with torch's own in-place operations: autograd refuses to go back through an operation that saved
+// it.  (A tensor made in inference mode has no such count.)
+void written(PyObject* o) {
+    if (o == Py_None) return;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
 // rows [R,V] that may lie further apart than V: the pointer, and the distance
 void* rows_of(const at::Tensor& t, const char* name, long long* stride) {
     if (!t.is_cuda()) {
@@ -410,6 +417,8 @@ struct LogprobOutputs {
         for (PyObject* o : made) Py_XDECREF(o);
     }
     PyObject* result(int rc) {
+        if (rc == S4C_OK)
+            for (PyObject* o : made) written(o);
         PyObject* t = PyTuple_New(5);
         for (int i = 0; i < 5; ++i) PyTuple_SET_ITEM(t, i, made[i]);
         return answer(rc, t);
@@ -507,10 +516,12 @@ PyObject* lm_head_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
             const Scratch scratch(a[11]);
             void* p = own.defined() ? own.data_ptr() : scratch.p;
             const size_t bytes = own.defined() ? (size_t)own.nbytes() : scratch.bytes;
-            return out.result(unlocked([&] {
+            const int rc = unlocked([&] {
                 return s4c_lm_head_greedy_logprobs(hidden, weight, tokens, R, V, H, temperature, top, out.logprob, out.entropy, out.top_token,
                                                    out.top_logprob, choice, max_logit, out.status, call_status, p, bytes, on.stream);
-            }));
+            });
+            if (rc == S4C_OK) written(a[10]), written(a[13]), written(a[14]);
+            return out.result(rc);
         } catch (...) {
             out.release();
             throw;
@@ -600,6 +611,8 @@ PyObject* distill(PyObject*, PyObject* const* a, Py_ssize_t n) {
                 return s4c_distill_topk(t.logits, t.stride, t.token, t.logit, t.K, t.labels, t.R, t.V, t.dt, t.temperature, t.teacher_weight, t.label_weight,
                                         loss, stats, scale, grad, distance, status, on.stream);
             });
+            if (rc == S4C_OK)
+                for (PyObject* o : made) written(o);
             PyObject* r = PyTuple_New(4);
             for (int i = 0; i < 4; ++i) PyTuple_SET_ITEM(r, i, made[i]);
             return answer(rc, r);
@@ -627,11 +640,12 @@ PyObject* distill_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
             long long distance = 0;
             void* g = t.grad(grad, &distance);
             const On on(t.x, a[10]);
-            return answer(unlocked([&] {
-                              return s4c_distill_topk_backward(t.logits, t.stride, t.token, t.logit, t.K, t.labels, t.R, t.V, t.dt, t.temperature,
-                                                               t.teacher_weight, t.label_weight, stats, grad_loss, g, distance, on.stream);
-                          }),
-                          grad);
+            const int rc = unlocked([&] {
+                return s4c_distill_topk_backward(t.logits, t.stride, t.token, t.logit, t.K, t.labels, t.R, t.V, t.dt, t.temperature, t.teacher_weight,
+                                                 t.label_weight, stats, grad_loss, g, distance, on.stream);
+            });
+            if (rc == S4C_OK) written(grad);
+            return answer(rc, grad);
         } catch (...) {
             Py_DECREF(grad);
             throw;

@@ -692,7 +692,9 @@ def distill_topk(logits, teacher_token=None, teacher_logit=None, labels=None, te
     """s4c_distill_topk: the loss of logits [R,V] against the teacher's ranked choices teacher_token / teacher_logit [R,K] and labels [R]
     -> dict(loss [R], stats [R,4], grad, status [R]).  ``grad``: None (loss alone), True (a new tensor) or a tensor [R,V] of the
     logits' type, the logits themselves among them; it receives row_scale[r] (None: 1) times the row's gradient in the same call.
-    In a program with autograd: ``logits.backward(out["grad"])``."""
+    In a program with autograd: ``logits.backward(out["grad"])`` (the loss itself has no graph).  A gradient in the logits' place changes them as
+    torch's in-place operations do: a backward pass that needs the values they had (an operation that saved its output, a soft
+    cap's tanh, say) is refused by autograd."""
     rc, (loss, stats, grad, status) = _bind.distill(logits, teacher_token, teacher_logit, labels, temperature, teacher_weight, label_weight, loss, stats,
                                                     grad, row_scale, status, stream)
     if rc:

@@ -1,0 +1,66 @@
+"""GPU: what the log-probability and distillation calls are to the program around them -- to autograd, the allocator, other streams and other threads."""
+import threading
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+def teacher(R, V, K, seed=1):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.randint(0, V, (R, K), generator=g, device="cuda", dtype=torch.int32), torch.randn(R, K, generator=g, device="cuda")
+
+
+@pytest.mark.parametrize("backward", [False, True])
+def test_a_gradient_in_the_place_of_saved_logits_is_refused_by_autograd(backward):
+    """A soft cap saves its output; the gradient written over it must not be taken for it on the way back."""
+    from paper_2506_14158_b200 import s4c
+
+    def head():
+        x = torch.randn(6, 301, device="cuda", generator=torch.Generator(device="cuda").manual_seed(2)).requires_grad_(True)
+        return x, 30 * torch.tanh(x / 30), torch.tanh(x / 30)
+
+    def grad(z, out):
+        if not backward:
+            return s4c.distill_topk(z, *teacher(6, 301, 4), grad=out)["grad"]
+        stats = s4c.distill_topk(z, *teacher(6, 301, 4))["stats"]
+        return s4c.distill_topk_backward(z, *teacher(6, 301, 4), stats, torch.ones(6, device="cuda"), grad=None if out is True else out)
+
+    x, z, _ = head()
+    g = grad(z, True)
+    z.backward(g)          # a gradient of its own: as ever
+    want = x.grad
+    x, z, _ = head()
+    before = z._version
+    g2 = grad(z, z.detach())
+    assert z._version > before and torch.equal(g2, g)
+    z.backward(g2)         # (the product saved no output: its logits may go)
+    assert torch.equal(x.grad, want)
+    x, _, capped = head()  # (tanh's own output)
+    g3 = grad(capped, capped.detach())
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        capped.backward(g3)
+
+
+def test_outputs_that_are_given_count_as_written():
+    from paper_2506_14158_b200 import s4c
+
+    R, V = 3, 40
+    x, i = torch.randn(R, V, device="cuda"), torch.zeros(R, dtype=torch.int32, device="cuda")
+    f, n = lambda *s: torch.empty(*s, device="cuda"), lambda *s: torch.empty(*s, dtype=torch.int32, device="cuda")
+    out = dict(logprob=f(R), entropy=f(R), top_token=n(R, 2), top_logprob=f(R, 2), status=n(R))
+    s4c.token_logprobs(x, i, 1.0, 2, **out)
+    assert all(t._version == 1 for t in out.values()) and x._version == 0
+    s4c.lm_head_logprobs(torch.zeros(R, 64, device="cuda").bfloat16(), torch.zeros(V, 64, device="cuda").bfloat16(), i, 1.0, 2, **out,
+                         choice=(c := n(R)), max_logit=(m := f(R)), call_status=(s := n(1)))
+    assert all(t._version == 2 for t in out.values()) and c._version == m._version == s._version == 1
+    d = dict(loss=f(R), stats=f(R, 4), status=n(R), grad=f(R, V))
+    s4c.distill_topk(x, *teacher(R, V, 3), **d)
+    assert all(t._version == 1 for t in d.values()) and x._version == 0
+    with torch.inference_mode():
+        y, out = torch.randn(R, V, device="cuda"), dict(logprob=f(R), entropy=f(R), status=n(R))
+    s4c.token_logprobs(y, i, **out)
+    s4c.distill_topk(y, *teacher(R, V, 3), grad=y)
+    torch.cuda.synchronize()
+    assert torch.isfinite(out["logprob"]).all()
