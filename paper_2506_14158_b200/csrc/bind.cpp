@@ -6,7 +6,6 @@
 
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
-#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -371,12 +370,21 @@ int size_of(int64_t n, const char* name) {
     }
     return (int)n;
 }
-// The stream of a call on the anchor's device, which is made current for the call.
+// The anchor's device and the call's stream, current from here to the end of the call: what the call makes is that stream's memory.  (Memory of the
+// current stream may be what an earlier tensor gave back while work of its own is still on its way there, which another stream does not wait for.)
 struct On {
     c10::cuda::CUDAGuard guard;
+    c10::cuda::OptionalCUDAStreamGuard other;
     void* stream;
-    On(const at::Tensor& anchor, PyObject* o)
-        : guard(anchor.device()), stream(o == Py_None ? (void*)c10::cuda::getCurrentCUDAStream(anchor.device().index()).stream() : stream_of(o)) {}
+    On(const at::Tensor& anchor, PyObject* o) : guard(anchor.device()) {
+        const auto device = anchor.device().index();
+        if (o == Py_None) {
+            stream = c10::cuda::getCurrentCUDAStream(device).stream();
+        } else {
+            stream = stream_of(o);
+            other.reset_stream(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(stream), device));
+        }
+    }
 };
 // Five outputs: logprob (where tokens are given), entropy [shape], top_token, top_logprob [shape, top] (where top > 0), status [shape]
 struct LogprobOutputs {
@@ -437,9 +445,9 @@ PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const int32_t* tokens = static_cast<const int32_t*>(beside(a[1], x, {R}, at::kInt, "tokens"));
         const float temperature = to_real(a[2]);
         const int top = to_integer(a[3]);
+        const On on(x, a[9]);
         LogprobOutputs out(a + 4, x, {R}, top, a[1] != Py_None);
         try {
-            const On on(x, a[9]);
             return out.result(unlocked([&] {
                 return s4c_token_logprobs(logits, stride, tokens, R, V, dt, temperature, top, out.logprob, out.entropy, out.top_token, out.top_logprob,
                                           out.status, on.stream);
@@ -470,9 +478,9 @@ PyObject* tree_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const int32_t* next_token = static_cast<const int32_t*>(beside(a[4], x, {B}, at::kInt, "next_token"));
         const float temperature = to_real(a[5]);
         const int top = to_integer(a[6]);
+        const On on(x, a[12]);
         LogprobOutputs out(a + 7, x, {B, entries}, top, true);
         try {
-            const On on(x, a[12]);
             return out.result(unlocked([&] {
                 return s4c_tree_logprobs(logits, tokens, walked, accept_len, next_token, B, T, V, entries - 1, dt, temperature, top, out.logprob,
                                          out.entropy, out.top_token, out.top_logprob, out.status, on.stream);
@@ -503,16 +511,12 @@ PyObject* lm_head_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
         int32_t* choice = static_cast<int32_t*>(beside(a[10], h, {R}, at::kInt, "choice"));
         float* max_logit = static_cast<float*>(beside(a[13], h, {R}, at::kFloat, "max_logit"));
         int32_t* call_status = static_cast<int32_t*>(beside(a[14], h, {1}, at::kInt, "call_status"));
+        const On on(h, a[12]);
         LogprobOutputs out(a + 5, h, {R}, top, a[2] != Py_None);
         try {
-            const On on(h, a[12]);
             at::Tensor own;
-            if (a[11] == Py_None) {
+            if (a[11] == Py_None)
                 own = unlocked([&] { return at::empty({(int64_t)s4c_lm_head_logprobs_workspace_bytes(R, V, H, top)}, h.options().dtype(at::kByte).requires_grad(false)); });
-                if (a[12] != Py_None && own.nbytes())  // (made on the current stream, used on another)
-                    c10::cuda::CUDACachingAllocator::recordStream(own.storage().data_ptr(),
-                                                                  c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(on.stream), h.device().index()));
-            }
             const Scratch scratch(a[11]);
             void* p = own.defined() ? own.data_ptr() : scratch.p;
             const size_t bytes = own.defined() ? (size_t)own.nbytes() : scratch.bytes;
@@ -585,6 +589,7 @@ PyObject* distill(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
         count(n, 13);
         const Teacher t(a);
+        const On on(t.x, a[12]);
         PyObject* made[4] = {};
         try {
             const auto keep = [&](int i, PyObject* given, at::IntArrayRef shape, at::ScalarType dtype) {
@@ -606,7 +611,6 @@ PyObject* distill(PyObject*, PyObject* const* a, Py_ssize_t n) {
             void* grad = made[2] == Py_None ? nullptr : t.grad(made[2], &distance);
             const float* scale = static_cast<const float*>(beside(a[10], t.x, {t.R}, at::kFloat, "row_scale"));
             int32_t* status = static_cast<int32_t*>(beside(made[3], t.x, {t.R}, at::kInt, "status"));
-            const On on(t.x, a[12]);
             const int rc = unlocked([&] {
                 return s4c_distill_topk(t.logits, t.stride, t.token, t.logit, t.K, t.labels, t.R, t.V, t.dt, t.temperature, t.teacher_weight, t.label_weight,
                                         loss, stats, scale, grad, distance, status, on.stream);
@@ -631,6 +635,7 @@ PyObject* distill_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
         tensor(a[7], "stats"), tensor(a[8], "grad_loss");
         const float* stats = static_cast<const float*>(beside(a[7], t.x, {t.R, 4}, at::kFloat, "stats"));
         const float* grad_loss = static_cast<const float*>(beside(a[8], t.x, {t.R}, at::kFloat, "grad_loss"));
+        const On on(t.x, a[10]);
         PyObject* grad = a[9];
         if (grad == Py_None)
             grad = THPVariable_Wrap(t.empty(t.x.sizes(), t.x.scalar_type()));
@@ -639,7 +644,6 @@ PyObject* distill_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
         try {
             long long distance = 0;
             void* g = t.grad(grad, &distance);
-            const On on(t.x, a[10]);
             const int rc = unlocked([&] {
                 return s4c_distill_topk_backward(t.logits, t.stride, t.token, t.logit, t.K, t.labels, t.R, t.V, t.dt, t.temperature, t.teacher_weight,
                                                  t.label_weight, stats, grad_loss, g, distance, on.stream);

@@ -64,3 +64,43 @@ def test_outputs_that_are_given_count_as_written():
     s4c.distill_topk(y, *teacher(R, V, 3), grad=y)
     torch.cuda.synchronize()
     assert torch.isfinite(out["logprob"]).all()
+
+
+CALLS = ["token_logprobs", "tree_logprobs", "lm_head_logprobs", "distill_topk", "distill_topk_backward"]
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_outputs_made_for_another_stream_are_that_streams(call):
+    """A tensor of the current stream is given back with work on its way into it; a call on another stream, which does not wait for that work, makes
+    outputs of the same sizes: none of them may lie there."""
+    from paper_2506_14158_b200 import s4c
+
+    R, V = 2000, 33
+    x, i = torch.randn(R, V, device="cuda"), torch.zeros(R, dtype=torch.int32, device="cuda")
+    tok, val = teacher(R, V, 3)
+    h, w = torch.randn(R, 64, device="cuda").bfloat16(), torch.randn(V, 64, device="cuda").bfloat16()
+    t4 = torch.zeros(20, 100, dtype=torch.int32, device="cuda")
+    paths = torch.full((20, 100), -1, dtype=torch.int32, device="cuda")
+    paths[:, 0] = 0
+    zero = torch.zeros(20, dtype=torch.int32, device="cuda")
+    st, scale = s4c.distill_topk(x, tok, val)["stats"], torch.ones(R, device="cuda")
+    run = {
+        "token_logprobs": lambda s: s4c.token_logprobs(x, i, 1.0, 2, stream=s),
+        "tree_logprobs": lambda s: s4c.tree_logprobs(x.view(20, 100, V), t4, paths, zero, zero, 1.0, 2, stream=s),
+        "lm_head_logprobs": lambda s: s4c.lm_head_logprobs(h, w, i, 1.0, 2, stream=s),
+        "distill_topk": lambda s: s4c.distill_topk(x, tok, val, grad=True, stream=s),
+        "distill_topk_backward": lambda s: dict(grad=s4c.distill_topk_backward(x, tok, val, st, scale, stream=s)),
+    }[call]
+    want = {k: v.clone() for k, v in run(None).items() if v is not None}
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    victims = [torch.empty_like(v) for v in want.values() for _ in range(3)]
+    torch.cuda._sleep(100_000_000)  # (about 50 ms in front of the writes below)
+    for v in victims:
+        v.fill_(9)
+    del v, victims
+    got = run(side)
+    side.synchronize()
+    torch.cuda.synchronize()
+    for k in want:
+        assert torch.equal(got[k], want[k]), k
