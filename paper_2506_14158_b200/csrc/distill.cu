@@ -559,7 +559,7 @@ static s4c_status ds_forward(const DsParams& p, long long rows, cudaStream_t str
     if (p.grad) {
         const int cluster = (int)std::min((long long)kMaxCluster, std::max((n + kDsSlice - 1) / kDsSlice, 4 * spare)), per = (int)((n + cluster - 1) / cluster);
         const size_t smem = (size_t)per * 16;
-        if (smem <= 200 * 1024)
+        if (smem <= kMaxRowSmem)
             return row_launch(distill_kernel<T, P, true, kDsKept, kDsKeptBlocks>, p, rows, cluster, per, kDsKept + 32, smem, stream);
     }
     // the loss alone, and rows that eight blocks cannot keep (the second look at them comes from L2, or memory)

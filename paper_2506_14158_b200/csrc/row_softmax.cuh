@@ -292,11 +292,13 @@ __device__ __forceinline__ float warp_sum(float v) {
 
 constexpr int kMaxCluster = 8;
 constexpr long long kSMs = 148;  // of a B200
+constexpr size_t kMaxRowSmem = 200 * 1024;  // dynamic shared memory of a block at most
 
 // `cluster` blocks for each row, as a cluster where they exchange anything
 template <typename Kernel, typename Params>
 static s4c_status row_launch(Kernel kernel, const Params& p, long long rows, int cluster, int per, int threads, size_t smem, cudaStream_t stream, bool exchange = true) {
-    if (smem > 32 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
+    // (always the same limit: the attribute is the kernel's, and another thread's call of another size may come between this line and the launch)
+    if (smem > 32 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMaxRowSmem) != cudaSuccess) {
         cudaGetLastError();
         return S4C_ERR_CUDA;
     }

@@ -104,3 +104,42 @@ def test_outputs_made_for_another_stream_are_that_streams(call):
     torch.cuda.synchronize()
     for k in want:
         assert torch.equal(got[k], want[k]), k
+
+
+def test_calls_of_different_sizes_from_several_threads():
+    """Kept rows of 35 KB and of 131 KB a block by one kernel, whose limit of shared memory is the kernel's, not the call's.  Through the C ABI, whose
+    calls run side by side."""
+    import ctypes
+
+    from paper_2506_14158_b200 import s4c
+    from paper_2506_14158_b200._build import lib_path
+
+    fn = ctypes.CDLL(lib_path()).s4c_distill_topk
+    vp, i, f, ll = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_longlong
+    fn.argtypes = [vp, ll, vp, vp, i, vp, i, i, i, f, f, f, vp, vp, vp, vp, ll, vp, vp]
+    p = lambda t: vp(t.data_ptr())
+    codes, start, rows, keep = [], threading.Barrier(6), [], []
+    for V in (262144, 70000) * 3:
+        x, grad, loss, stats = torch.randn(1, V, device="cuda"), torch.empty(1, V, device="cuda"), torch.zeros(1, device="cuda"), torch.zeros(1, 4, device="cuda")
+        tok, val = teacher(1, V, 3)
+        want = s4c.distill_topk(x, tok, val, grad=True)
+        stream = torch.cuda.Stream()
+        args = (p(x), ll(V), p(tok), p(val), i(3), None, i(1), i(V), i(0), f(1.0), f(1.0), f(1.0), p(loss), p(stats), None, p(grad), ll(V), None, vp(stream.cuda_stream))
+        rows.append((args, want["loss"], loss, want["grad"], grad))
+        keep.append((x, stats, tok, val, stream))
+    torch.cuda.synchronize()
+
+    def calls(args):
+        start.wait()
+        for _ in range(400):
+            codes.append(fn(*args))
+
+    threads = [threading.Thread(target=calls, args=(r[0],)) for r in rows]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert len(codes) == 2400 and codes.count(0) == 2400, codes.count(7)
+    for _, want, loss, want_grad, grad in rows:
+        assert torch.equal(want, loss) and torch.equal(want_grad, grad)
