@@ -32,6 +32,7 @@ EXPORTS = ["s4c_version", "s4c_status_string", "s4c_tree_attention_workspace_byt
            "s4c_token_logprobs", "s4c_tree_logprobs", "s4c_lm_head_logprobs_workspace_bytes", "s4c_lm_head_logprobs", "s4c_lm_head_greedy_logprobs", "s4c_distill_topk",
            "s4c_distill_topk_backward"]
 NOALLOC_SCRATCH_BYTES = 1 << 20
+MAX_TOP_LOGPROBS, MAX_TOP_HEAD = 64, 8  # alternatives from logits in memory; those of the LM head
 
 
 class S4CError(RuntimeError):

@@ -66,11 +66,14 @@ class TargetVerify:
     """Buffers for one greedy verify step of B sequences with T-node trees; ``forward`` runs the chain above and can be
     captured in a CUDA graph (all buffers are allocated here, once; the caches are the caller's and are written in place).
     ``keep`` keeps every layer's intermediate rows (for tests); otherwise two sets of row buffers alternate.
-    ``top_logprobs`` (None: none; 0: no alternatives): the pass also returns what the target's distributions say (see ``forward``)."""
+    ``top_logprobs`` (None: none; 0: no alternatives): the pass also returns what the target's distributions say (see ``forward``); at most 8
+    alternatives on the greedy route, 64 on the sampling route (a pass built for sampling with more than 8 refuses temperature 0)."""
 
     def __init__(self, w: TargetWeights, B: int, T: int, Hq: int, Hkv: int, d: int, C: int, k_caches, v_caches, max_depth: int,
                  eps: float = 1e-5, rope_theta: float = 10000.0, keep: bool = False, stochastic: bool = False,
                  top_logprobs: Optional[int] = None):
+        if top_logprobs is not None and not 0 <= top_logprobs <= (s4c.MAX_TOP_LOGPROBS if stochastic else s4c.MAX_TOP_HEAD):
+            raise ValueError(f"top_logprobs must be 0 to {s4c.MAX_TOP_HEAD} on the greedy route, to {s4c.MAX_TOP_LOGPROBS} on the sampling route")
         self.w, self.B, self.T, self.Hq, self.Hkv, self.d, self.C = w, B, T, Hq, Hkv, d, C
         self.eps, self.rope_theta, self.max_depth = eps, rope_theta, max_depth
         self.k_caches, self.v_caches = list(k_caches), list(v_caches)
@@ -138,6 +141,8 @@ class TargetVerify:
         status) per emitted token [B,max_depth+1], at the pass's temperature (s4c_tree_logprobs); on the greedy route dict(entropy,
         top_token, top_logprob, status) per node [B,T], at temperature 1 -- the token emitted after node i is the target's choice there,
         top_token[b,i,0]; the alternatives are also what a drafter's head at that node learns from (`DrafterHead.objective`)."""
+        if self.top_logprobs is not None and self.top_logprobs > s4c.MAX_TOP_HEAD and not temperature > 0.0:
+            raise ValueError(f"a greedy pass has at most {s4c.MAX_TOP_HEAD} alternatives, this one was built for {self.top_logprobs}")
         w, B, T = self.w, self.B, self.T
         n = len(w.layers)
         s4c.embed_gather(w.embedding, tokens.reshape(-1), out=self.x[0])

@@ -130,8 +130,13 @@ class VerifyStep:
 
     def set_logprobs(self, top: Optional[int], temperature: Optional[float] = None):
         """From now on ``run()`` also says what the target's distribution at every emitted token was (s4c_tree_logprobs: log probability,
-        entropy, ``top`` alternatives, in ``self.logprobs``); ``top=None`` goes back.  ``temperature``: the step's, or 1 for greedy steps.
-        A step captured or bound to host inputs before goes on as it was (its outputs stay allocated)."""
+        entropy, ``top`` alternatives (64 at most), in ``self.logprobs``); ``top=None`` goes back.  ``temperature``: the step's, or 1 for greedy
+        steps.  A step captured or bound to host inputs before goes on as it was (its outputs stay allocated).  It is the distribution of all
+        of the vocabulary also where the step samples from a filtered one (``set_filter``)."""
+        if top is not None and not 0 <= top <= s4c.MAX_TOP_LOGPROBS:
+            raise ValueError(f"top must be 0 to {s4c.MAX_TOP_LOGPROBS}")
+        if temperature is not None and not 0.0 < temperature < float("inf"):
+            raise ValueError("temperature must be positive and finite")
         self.top_logprobs = None if top is None else int(top)
         if top is None:
             return

@@ -1,0 +1,24 @@
+"""What the verify pass and step refuse of log probabilities when they are asked for, not when they run (no GPU needed)."""
+import pytest
+
+
+def test_a_pass_refuses_alternatives_that_its_route_has_not(s4c_lib):
+    from paper_2506_14158_b200 import target
+
+    for top, stochastic in [(9, False), (20, False), (-1, False), (65, True), (-1, True)]:
+        with pytest.raises(ValueError, match="top_logprobs must be 0 to 8"):
+            target.TargetVerify(None, 1, 8, 4, 2, 64, 64, [], [], 4, stochastic=stochastic, top_logprobs=top)
+    one = object.__new__(target.TargetVerify)
+    one.top_logprobs = 20
+    with pytest.raises(ValueError, match="at most 8 alternatives"):
+        one.forward(None, None, None, temperature=0.0)
+
+
+def test_a_step_refuses_what_its_run_would(s4c_lib):
+    from paper_2506_14158_b200.verify import VerifyStep
+
+    step = object.__new__(VerifyStep)
+    for kw in (dict(top=65), dict(top=-1), dict(top=3, temperature=0.0), dict(top=3, temperature=float("inf")), dict(top=3, temperature=float("nan"))):
+        with pytest.raises(ValueError):
+            step.set_logprobs(**kw)
+    assert not vars(step)
