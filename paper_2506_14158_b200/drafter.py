@@ -84,7 +84,7 @@ class DrafterHead:
         if train:  # the head's logits exist in memory for its objective only
             f32 = dict(dtype=torch.float32, device=dev)
             self.logits, self.loss, self.stats = torch.empty(R, V, **f32), torch.empty(R, **f32), torch.empty(R, 4, **f32)
-            self.status_objective = torch.empty(R, **i32)
+            self.status_objective, self.status_logits = torch.empty(R, **i32), torch.zeros(1, **i32)
             self.ws_logits = torch.empty(max(1, s4c.lm_head_logits_workspace_bytes(R, V, H)), dtype=torch.uint8, device=dev)
 
     def forward(self, tokens: torch.Tensor, features: torch.Tensor, cache_len: torch.Tensor, parent: torch.Tensor,
@@ -120,14 +120,15 @@ class DrafterHead:
         """What the head's last ``forward`` is worth as training (Section 3.1.2: cross entropy against the target's distribution, weight 1,
         and against the text, weight 0.1): its logits (s4c_lm_head_logits) against the target's ranked choices per row [B*T, K] -- what
         `TargetVerify(top_logprobs=K)` returns for the nodes -- and, where given, the text's next tokens [B*T] (s4c_distill_topk).
-        A head built with ``train=True``.  Returns dict(loss [B*T], logits [B*T,V], status [B*T]); ``grad``: the gradient of
+        A head built with ``train=True``.  Returns dict(loss [B*T], logits [B*T,V], status [B*T], status_logits [1] (of the product that makes the
+        logits; ``status_head`` stays the forward's)); ``grad``: the gradient of
         sum(row_scale * loss) stands in the place of the logits (key "grad"), for the caller's own backward pass through the LM head."""
         if not self.train:
             raise ValueError("build the head with train=True to ask for its objective")
-        s4c.lm_head_logits(self.f_out, self.w.lm_head, self.logits, self.status_head, self.ws_logits)
+        s4c.lm_head_logits(self.f_out, self.w.lm_head, self.logits, self.status_logits, self.ws_logits)
         s4c.distill_topk(self.logits, teacher_token, teacher_logit, labels, temperature, teacher_weight, label_weight,
                          grad=self.logits if grad else None, row_scale=row_scale, loss=self.loss, stats=self.stats, status=self.status_objective)
-        return {"loss": self.loss, "grad" if grad else "logits": self.logits, "status": self.status_objective}
+        return {"loss": self.loss, "grad" if grad else "logits": self.logits, "status": self.status_objective, "status_logits": self.status_logits}
 
 
 class MultiHeadDrafter:
