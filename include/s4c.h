@@ -433,7 +433,7 @@ s4c_status s4c_lm_head_greedy_logprobs(const void* hidden, const void* weight, c
  *   status [R] int32 or NULL: S4C_SEQ_TOKEN_RANGE (a teacher's token or a label outside [-1, V)), S4C_SEQ_NONFINITE (a NaN, a +Inf or
  *                 nothing but -Inf in the logits of a row that has something to learn; a NaN or +Inf teacher logit).  Such a row's loss and
  *                 gradient are NaN.
- *   A term whose weight is 0 is not looked at.  Weights are finite, temperature as above and below 1e18.
+ *   A term whose weight is 0 is not looked at.  Weights are finite, with a gradient teacher_weight times temperature too; temperature as above and below 1e18.
  * s4c_distill_topk_backward writes grad = grad_loss[r] times the same gradient from the stats that s4c_distill_topk left for
  * the same logits, teacher, labels, temperature and weights (one more pass over the logits, which are read only).
  * Sums are float32, the losses' terms float64; results do not depend on timing.  A row's sums may be taken in another order

@@ -595,7 +595,8 @@ static s4c_status ds_check(const void* logits, long long row_stride, const int32
                            s4c_dtype dt, float temperature, float teacher_weight, float label_weight, const void* grad, long long grad_stride) {
     if (!logits || (K > 0 && (!teacher_token || !teacher_logit))) return S4C_ERR_NULL;
     if (R < 0 || R > S4C_MAX_LOGITS_ROWS || V < 1 || V > S4C_MAX_LOGITS_COLUMNS || row_stride < V || K < 0 || !(temperature > 0.0f) || !(temperature < 1e18f) ||
-        !(kLog2E / temperature < INFINITY) || !(fabsf(teacher_weight) < INFINITY) || !(fabsf(label_weight) < INFINITY) || (grad && grad_stride < V))
+        !(kLog2E / temperature < INFINITY) || !(fabsf(teacher_weight) < INFINITY) || !(fabsf(label_weight) < INFINITY) ||
+        (grad && (grad_stride < V || !(fabsf(teacher_weight * temperature) < INFINITY))))
         return S4C_ERR_SHAPE;
     if (dt != S4C_F32 && dt != S4C_BF16) return S4C_ERR_DTYPE;
     if (K > kDsMaxTeach) return S4C_ERR_UNSUPPORTED;

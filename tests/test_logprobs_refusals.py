@@ -22,3 +22,16 @@ def test_a_step_refuses_what_its_run_would(s4c_lib):
         with pytest.raises(ValueError):
             step.set_logprobs(**kw)
     assert not vars(step)
+
+
+def test_a_gradient_whose_weight_leaves_float32_is_refused(s4c_lib):
+    """The gradient's coefficient is teacher_weight temperature: beyond float32 every entry would be infinite or NaN."""
+    from test_abi_logprobs import P, _entry
+
+    far = 1 << 30
+    fwd = _entry(s4c_lib, "s4c_distill_topk", [("x", P), ("ld", 100), ("tt", P), ("tl", P), ("K", 8), ("c", None), ("R", 3), ("V", 100), ("dt", 0),
+                                            ("tau", 1e10), ("wt", 1e30), ("wl", 1.0), ("loss", P), ("stats", None), ("g", None), ("grad", far), ("gld", 100),
+                                            ("st", None), ("s", None)])
+    bwd = _entry(s4c_lib, "s4c_distill_topk_backward", [("x", P), ("ld", 100), ("tt", P), ("tl", P), ("K", 8), ("c", None), ("R", 3), ("V", 100), ("dt", 0),
+                                                     ("tau", 1e10), ("wt", -1e30), ("wl", 1.0), ("stats", P), ("g", P), ("grad", far), ("gld", 100), ("s", None)])
+    assert fwd() == 2 and bwd() == 2 and fwd(wt=-1e30) == 2
