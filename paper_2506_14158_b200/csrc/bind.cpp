@@ -518,6 +518,7 @@ PyObject* lm_head_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
             if (a[11] == Py_None)
                 own = unlocked([&] { return at::empty({(int64_t)s4c_lm_head_logprobs_workspace_bytes(R, V, H, top)}, h.options().dtype(at::kByte).requires_grad(false)); });
             const Scratch scratch(a[11]);
+            if (a[11] != Py_None) same_device(tensor(a[11], "workspace"), h, "workspace");
             void* p = own.defined() ? own.data_ptr() : scratch.p;
             const size_t bytes = own.defined() ? (size_t)own.nbytes() : scratch.bytes;
             const int rc = unlocked([&] {

@@ -143,3 +143,13 @@ def test_calls_of_different_sizes_from_several_threads():
     assert len(codes) == 2400 and codes.count(0) == 2400, codes.count(7)
     for _, want, loss, want_grad, grad in rows:
         assert torch.equal(want, loss) and torch.equal(want_grad, grad)
+
+
+@pytest.mark.skipif(torch.cuda.device_count() < 2, reason="a workspace on another device takes two")
+def test_a_workspace_on_another_device_is_refused():
+    from paper_2506_14158_b200 import s4c
+
+    h, w = torch.zeros(4, 64, device="cuda:0").bfloat16(), torch.zeros(100, 64, device="cuda:0").bfloat16()
+    ws = torch.empty(s4c.lm_head_logprobs_workspace_bytes(4, 100, 64, 2), dtype=torch.uint8, device="cuda:1")
+    with pytest.raises(ValueError, match="workspace is on cuda:1"):
+        s4c.lm_head_logprobs(h, w, None, 1.0, 2, workspace=ws)
