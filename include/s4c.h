@@ -359,7 +359,8 @@ s4c_status s4c_lm_head_logits(const void* hidden, const void* weight, int R, int
  * Exponentials and sums are float32, a row's last steps float64; results do not depend on timing (in calls of few rows, and for
  * rows that start elsewhere in a 16-byte word, a row's sums may be taken in another order).
  *   logprob, entropy [n] f32, top_token [n,top] int32, top_logprob [n,top] f32, status [n] int32 (each row's S4C_SEQ_* flags),
- *   any of logprob, entropy, status may be NULL, top_token and top_logprob iff top is 0.
+ *   any of logprob, entropy, status may be NULL (logprob not in s4c_tree_logprobs, whose tokens are always given), top_token and
+ *   top_logprob iff top is 0.
  *   Logits of -Inf are masked: probability 0, never an alternative; where fewer than `top` tokens are left the others are
  *   -1 with log probability -Inf, and a given token that is masked has log probability -Inf.
  *   Token -1: a row that is not asked for (padding).  What it holds does not matter; logprob and entropy 0, alternatives -1 / -Inf, status 0.
