@@ -6,12 +6,12 @@
 // The gradient is dense in p and p1 and sparse in q: a pass over the row writes a exp((z_v - m) / tau) + b exp(z_v - m), and the
 // at most K + 1 places that q and the label touch are written once more, behind a barrier.
 //
-// Loss and gradient in one call read and write every logit once (4096 x 128256 bf16 rows, K = 100, labels: 430 to 480 us, 68 to 75 % of the copy
+// Loss and gradient in one call read and write every logit once (4096 x 128256 bf16 rows, K = 100: 440 to 475 us from box to box, 68 to 73 % of the copy
 // bandwidth; the exponentials take 59 % of their unit, all instructions 55 % of their slots).  A cluster of up to eight blocks takes a row; its logits are
 // copied to shared memory (cp.async, each thread's vectors for that thread alone, so that no barrier stands between a copy and its use), summed
 // there against running references, and read from there once more for the gradient.  The blocks exchange (m, S, S1) through each
 // other's shared memory.  The teacher's K entries are one warp's work, beside the stream.  The loss alone streams (2048 x 128256:
-// 86 us, 93 % of the copy bandwidth), and so does the backward pass, whose blocks start from the row's saved (m, 1/S, 1/S1): 167 us, 96 %.
+// 86 us, 94 % of the copy bandwidth), and so does the backward pass, whose blocks start from the row's saved (m, 1/S, 1/S1): 167 us, 96 %.
 #include <algorithm>
 #include <type_traits>
 
@@ -26,17 +26,18 @@ constexpr int kDsBatch = 4;             // vectors that a thread takes at once
 constexpr float kDsSlack = 8.0f;        // how far (log2) a maximum may pass the reference of a running sum
 // Threads of a block's stream (one warp more has the teacher) and blocks of an SM, where the row is kept in shared memory, where it is streamed,
 // and for short rows.  What a warp does besides its stream is a third of its instructions where the row is kept, so few warps are better
-// there (4096 x 128256 bf16, loss and gradient: 256 threads 513 us, 192 495 us, 128 438 us); a stream wants more of them (the loss
-// alone 107 us with 6 x 128 threads for 2048 rows, 87 us with 5 x 256); a short row is two warps' (8000 x 4000: 51 us by 8 x 64, 68 by 16 x 32).
+// there (4096 x 128256 bf16, loss and gradient: 256 threads 513 us, 192 495 us, 128 438 us when they were compared); a stream wants more of them
+// (the loss alone 107 us with 6 x 128 threads for 2048 rows, 87 us with 5 x 256); a short row is two warps' (8000 x 4000, not in L2: 62 us by 8 x 64, 78 by
+// 16 x 32).
 constexpr int kDsKept = 128, kDsKeptBlocks = 6, kDsStreamed = 256, kDsStreamedBlocks = 5, kDsShort = 64, kDsShortBlocks = 8;
 // Vectors of a block's share of a kept row, as far as eight blocks suffice: 34 KB, the most that leaves room for six blocks of an SM.  (2000 x 65536
 // bf16, loss and gradient: 128 us by five blocks of 2048 vectors at most, 114 us by four of 2049; 132 us by 1536)
 constexpr int kDsSlice = 2144;
-// Vectors of a short row at most, and in calls of no more rows than SMs (30 x 8000: 7.4 us as short rows, 5.8 us by two blocks; 2000 x 5000: 17 us as
-// short rows, 22 us as kept ones)
+// Vectors of a short row at most, and in calls of no more rows than SMs (not in L2: 30 x 8000 8.4 us as short rows, 5.8 us by blocks of a cluster;
+// 2000 x 5000 22 us as short rows, 27 us as kept ones)
 constexpr int kDsShortRow = 1024, kDsShortFew = 512;
 // How 2^(x log2 e), of the label's term, comes from 2^(x log2 e / tau): there is none or it is the same, by an exponential of its own, or squared once
-// or twice (tau = 2 or 4: two exponentials per logit and pass bound the kernel otherwise -- 2048 x 32000 bf16 rows with labels, tau = 2: 83 us by
+// or twice (tau = 2 or 4: two exponentials per logit and pass bound the kernel otherwise -- 2048 x 32000 bf16 rows with labels, tau = 2: 84 us by
 // exponentials of their own, 70 us squared)
 enum { kDsOne = 0, kDsTwo = -1, kDsSquare = 1, kDsFourth = 2 };
 enum { kDsSkip = 0, kDsRow = 1, kDsBad = 2 };  // what stats[3] says of a row: nothing to learn from, a loss, undefined

@@ -3,9 +3,10 @@
 //
 // With m = max_v x_v, y_v = (x_v - m) / tau and S = sum_v exp(y_v):
 //     log p(t) = y_t - ln S,   H = ln S - (sum_v exp(y_v) y_v) / S,
-// differences against the maximum throughout, so that neither large logits nor small temperatures lose the small terms.
+// sums of differences against a logit of the row: in the stream against a reference that lies at most 8 powers of two below the maximum (ln S is up to 5.5 more
+// than against the maximum itself, its rounding 2^-24 of that), in extreme rows against the maximum.
 //
-// HBM-bound: every logit is read once, by a stream that no barrier interrupts (2048 x 128256 bf16 rows: 92 us, 88 % of the copy bandwidth, and 105
+// HBM-bound: every logit is read once, by a stream that no barrier interrupts (2048 x 128256 bf16 rows: 93 us, 87 % of the copy bandwidth, and 106
 // with eight alternatives; one row of 32000 float32 logits 4.6 us, and 7.2).  A block (a cluster of up to eight for few rows) takes a
 // row; its threads keep running sums S = sum 2^y and E = sum 2^y y against a reference of their own, y = x log2(e) / tau - M, and raise M only
 // when a vector's maximum passes it by 2^8 (exact in any case; it spares the rescaling of nearly every vector).  Elements travel in pairs
@@ -116,7 +117,9 @@ struct alignas(16) LpShared {
     __device__ __forceinline__ uint64_t* candidates() { return reinterpret_cast<uint64_t*>(ring); }
 };
 
-// Where the candidates overflow: the top-th greatest logit and, among its equals, the highest token that still belongs, by bisection.
+// Where the candidates overflow: the top-th greatest logit and, among its equals, the highest token that still belongs, by bisection.  About fifty passes
+// over the block's share: 2048 x 128256 bf16 rows filled with -1e4 but for three tokens, five alternatives, 9.5 ms (three alternatives, or a fill
+// of -Inf, which is no candidate: 100 us); 26 x 32000 float32 170 us.
 template <typename T, int S>
 struct LpExactly {
     // How many of the block's logits pass `f(ordered bits, token)`; -Inf and NaN never do.  `turn` alternates between calls.
@@ -500,9 +503,9 @@ static s4c_status lp_launch(const LpParams& p, long long rows, cudaStream_t stre
     const int cluster = (int)std::max(1ll, std::min({p.top ? 4ll : (long long)kMaxCluster, 2 * kSMs / rows, n / 2048}));
     const int per = (int)((n + cluster - 1) / cluster);
     // Shorter rows by fewer threads each and more rows at once: what a block does behind its stream is the same for every warp.  (4000 bf16 rows, five
-    // alternatives, by 64 / 128 / 256 threads: V = 2000 27 / 31 / 62 us, 4000 34 / 32 / 56, 16384 52 / 51 / 68, 32000 75 / 66 / 84; 1777 of 50001 53 / 51 / 52,
-    // 2368 of 128256 117 by 128, 112 by 256.  140 rows of 32000: 13 / 11 / 10.  More than a quarter as many alternatives as threads lie far below the
-    // threads' maxima: 4000 x 2000, 64 alternatives 150 / 52 / 85 us.)
+    // alternatives, by 64 / 128 / 256 threads, each call on rows that are not in L2: V = 2000 29 / 32 / 64 us, 4000 35 / 33 / 57, 16384 52 / 51 / 68,
+    // 32000 75 / 67 / 84; 1777 of 50001 53 / 51 / 51, 2368 of 128256 120 / 116 / 114.  140 rows of 32000: 15 / 12 / 11.  More than a quarter as many alternatives as threads lie far below the
+    // threads' maxima: 4000 x 2000, 64 alternatives, rows in L2, 150 / 52 / 86 us.)
     if (n <= kLpShortRow && p.top <= kLpShort / 4) return row_launch(logprobs_kernel<T, kLpShort, kLpShortBlocks>, p, rows, 1, (int)n, kLpShort, 0, stream);
     if (n <= (rows > kSMs ? kLpMediumRow : kLpMediumFew))
         return row_launch(logprobs_kernel<T, kLpMedium, kLpMediumBlocks>, p, rows, 1, (int)n, kLpMedium, 0, stream);
