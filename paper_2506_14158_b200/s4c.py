@@ -641,7 +641,8 @@ _LOGPROB_OUTPUTS = ("logprob", "entropy", "top_token", "top_logprob", "status")
 def token_logprobs(logits, tokens=None, temperature: float = 1.0, top: int = 0, logprob=None, entropy=None, top_token=None,
                    top_logprob=None, status=None, stream=None):
     """s4c_token_logprobs: logits [R,V] float32 or bfloat16 (rows may lie further apart than V), tokens [R] int32 (-1: a row that is not
-    asked for) or None -> dict(logprob [R] (None without tokens), entropy [R], top_token / top_logprob [R,top] (None for top 0), status [R])."""
+    asked for) or None -> dict(logprob [R] (None without tokens), entropy [R], top_token / top_logprob [R,top] (None for top 0), status [R]).
+    Here and in the calls below, outputs that are not given are made in the memory of ``stream`` (None: the current one)."""
     rc, out = _bind.token_logprobs(logits, tokens, temperature, top, logprob, entropy, top_token, top_logprob, status, stream)
     if rc:
         raise S4CError("s4c_token_logprobs", rc)

@@ -140,7 +140,7 @@ class TargetVerify:
         A pass built with ``top_logprobs`` also returns logprobs: on the sampling route dict(logprob, entropy, top_token, top_logprob,
         status) per emitted token [B,max_depth+1], at the pass's temperature (s4c_tree_logprobs); on the greedy route dict(entropy,
         top_token, top_logprob, status) per node [B,T], at temperature 1 -- the token emitted after node i is the target's choice there,
-        top_token[b,i,0]; the alternatives are also what a drafter's head at that node learns from (`DrafterHead.objective`)."""
+        top_token[b,i,0], its log probability top_logprob[b,i,0] (so ask for one alternative at least where they are wanted); the alternatives are also what a drafter's head at that node learns from (`DrafterHead.objective`)."""
         if self.top_logprobs is not None and self.top_logprobs > s4c.MAX_TOP_HEAD and not temperature > 0.0:
             raise ValueError(f"a greedy pass has at most {s4c.MAX_TOP_HEAD} alternatives, this one was built for {self.top_logprobs}")
         w, B, T = self.w, self.B, self.T

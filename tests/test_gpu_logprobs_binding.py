@@ -153,3 +153,35 @@ def test_a_workspace_on_another_device_is_refused():
     ws = torch.empty(s4c.lm_head_logprobs_workspace_bytes(4, 100, 64, 2), dtype=torch.uint8, device="cuda:1")
     with pytest.raises(ValueError, match="workspace is on cuda:1"):
         s4c.lm_head_logprobs(h, w, None, 1.0, 2, workspace=ws)
+
+
+@pytest.mark.parametrize("call", ["token_logprobs", "lm_head_logprobs", "distill_topk"])
+def test_a_captured_call_on_a_named_stream_makes_the_graphs_memory(call):
+    """Outputs and workspaces made under capture, on the capturing stream given by name, and on one that was forked from it, live in the graph."""
+    from paper_2506_14158_b200 import s4c
+
+    R, V = 50, 3001
+    x, i = torch.randn(R, V, device="cuda"), torch.zeros(R, dtype=torch.int32, device="cuda")
+    h, w = torch.randn(R, 64, device="cuda").bfloat16(), torch.randn(V, 64, device="cuda").bfloat16()
+    tok, val = teacher(R, V, 3)
+    run = {"token_logprobs": lambda s: s4c.token_logprobs(x, i, 1.0, 2, stream=s), "lm_head_logprobs": lambda s: s4c.lm_head_logprobs(h, w, i, 1.0, 2, stream=s),
+           "distill_topk": lambda s: s4c.distill_topk(x, tok, val, grad=True, stream=s)}[call]
+    run(None)
+    torch.cuda.synchronize()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph):
+        here = torch.cuda.current_stream()
+        a = run(here)
+        side.wait_stream(here)
+        b = run(side)
+        here.wait_stream(side)
+    others = [torch.full((R, V), 9.0, device="cuda") for _ in range(8)] + [torch.full((R,), 9, device="cuda") for _ in range(64)]
+    for t in (x, h):
+        t.copy_(torch.randn_like(t))
+    graph.replay()
+    torch.cuda.synchronize()
+    want = run(None)
+    assert all((t == 9).all() for t in others)
+    for k, v in want.items():
+        if v is not None:
+            assert torch.equal(a[k], v) and torch.equal(b[k], v), k

@@ -88,3 +88,17 @@ def test_the_lm_head_at_the_ends_of_the_temperatures(R, V):
         tau = float(np.float32(tau))
         got = s4c.lm_head_logprobs(h.cuda(), w.cuda(), torch.from_numpy(tok).cuda(), tau, 5)
         check(got, oracle.token_logprobs(x, tok, tau, 5), V, 5)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [97, 5001, 70001])
+def test_masks_of_both_kinds_around_one_token(dtype, V):
+    """Threads that meet nothing but -inf and the type's lowest value, beside the one that has the row's maximum."""
+    n, low = np.arange(V), float(torch.finfo(TYPES[dtype]).min)
+    mixed = np.where(n % 2 == 0, low, -np.inf)
+    x = np.stack([np.where(n == 1, 0.0, mixed), np.where(n == V - 1, -3.0, mixed), np.where(n == V // 2, 1e36, mixed), np.where(n == 3, -1e36, mixed)])
+    x = torch.from_numpy(x.astype(np.float32)).to(TYPES[dtype])
+    tok = np.array([1, 2, V // 2, 0])
+    for tau in (0.5, 1.0, 2.0, 100.0, 1e20, 1e29, 2e30, 3e38):
+        tau = float(np.float32(tau))
+        check(run(x.cuda(), tok, tau, 3), oracle.token_logprobs(x.double().numpy(), tok, tau, 3), V, 3)
