@@ -6,7 +6,7 @@
 // The gradient is dense in p and p1 and sparse in q: a pass over the row writes a exp((z_v - m) / tau) + b exp(z_v - m), and the
 // at most K + 1 places that q and the label touch are written once more, behind a barrier.
 //
-// Loss and gradient in one call read and write every logit once (4096 x 128256 bf16 rows, K = 100: 440 to 475 us from box to box, 68 to 73 % of the copy
+// Loss and gradient in one call read and write every logit once (4096 x 128256 bf16 rows, K = 100: 440 to 475 us from GPU to GPU, 68 to 73 % of the copy
 // bandwidth; the exponentials take 59 % of their unit, all instructions 55 % of their slots).  A cluster of up to eight blocks takes a row; its logits are
 // copied to shared memory (cp.async, each thread's vectors for that thread alone, so that no barrier stands between a copy and its use), summed
 // there against running references, and read from there once more for the gradient.  The blocks exchange (m, S, S1) through each
